@@ -31,6 +31,7 @@ from .bart import BART_EINVAL, BartError, _check
 
 BART_F32, BART_F16, BART_BF16 = 0, 1, 2
 BART_MAX_TOP = 64
+MAX_CLASSES = 1 << 30
 STATE_BLOCK = 256
 _DTYPES = {torch.float32: BART_F32, torch.float16: BART_F16, torch.bfloat16: BART_BF16}
 
@@ -122,6 +123,8 @@ def _rows(scores, labels, mask, temperature) -> Rows:
         _refuse(f"scores must be float32, float16 or bfloat16, not {scores.dtype}")
     if not scores.is_cuda:
         _refuse("scores must be on a HIP device")
+    if not 1 <= c <= MAX_CLASSES:   # the library's field is narrower than a tensor's size
+        _refuse(f"scores must have 1 to 2^30 classes, not {c}")
     if c > 1 and scores.stride(1) != 1:
         _refuse("the classes of a row must be next to each other (stride 1)")
     r = Rows(scores.data_ptr(), n, scores.stride(0) if n > 1 else c, c, dtype, None, 0, None, 0,
