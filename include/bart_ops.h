@@ -92,8 +92,8 @@ typedef struct {
  *  - label < 0: logp 0, and w counts as 0; where w and h are 0 the whole row's
  *    gradient is 0 (also where the row is NaN);
  *  - label not allowed or its score -inf: logp -inf;
- *  - label >= n_class: logp NaN, and with w_logp the gradient NaN at allowed
- *    places above -inf;
+ *  - label >= n_class: logp NaN, and where w is not 0 the gradient NaN at
+ *    allowed places above -inf;
  *  - a weight that is not finite (or overflows over T): the gradient NaN at
  *    allowed places above -inf;
  *  - fewer than k allowed scores above -inf: the rest of the alternatives are

@@ -609,7 +609,7 @@ __device__ __forceinline__ RowGrad row_grad(const RowsArgs &A, int64_t i, int64_
   q.M = ref_of(r.m, q.a);
   const bool big = fabsf(q.M) >= kMostRef;
   q.kind = (w == 0.f && h == 0.f) || r.logs == kNegInf ? 0 : r.logs != r.logs ? 2 : big ? 3 : 1;
-  if (A.g.w_logp && label >= A.r.n_class) q.kind = 2;
+  if (w != 0.f && label >= A.r.n_class) q.kind = 2;
   q.nl2 = -r.logs * kLog2e;
   if (q.kind == 1) q.nl2 -= __builtin_fmaf(r.m, q.a, -q.M);
   const float p0 = exp2_fast(q.nl2);  // 1 / s
