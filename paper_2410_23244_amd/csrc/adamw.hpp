@@ -3,6 +3,7 @@
 // element, 5.25 TB/s); 3e8 bf16 elements with 8-bit states 525 to 580 us (10.06
 // bytes, 5.2 to 5.7 TB/s, 56 instructions an element beside it).
 #pragma once
+#include <float.h>
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -222,8 +223,10 @@ __device__ __forceinline__ void adamw_chunk(const bart_adamw_tensor &t, int64_t 
       least = min(least, __float_as_uint(v[n][e]) - 1);
     }
     // the root that is held in 8 bits is rounded correctly, so that its code is
-    // that of the definition; where only the update uses it, 1 ulp serves
-    if (BITS == 8 && __any(least < __float_as_uint(kRootFrom) - 1)) {
+    // that of the definition; where only the update uses it, 1 ulp serves, but
+    // the hardware's root takes what is below the normal range as 0
+    constexpr float kFrom = BITS == 8 ? kRootFrom : FLT_MIN;
+    if (__any(least < __float_as_uint(kFrom) - 1)) {
 #pragma unroll
       for (int e = 0; e < G; ++e) r[e] = sqrtf(v[n][e]);
     } else {
