@@ -47,12 +47,14 @@ class Calibration:
         self._dD, self._db = zeros(n_class, n_class), zeros(n_class)
         self.opt = ops.AdamW(self.D + self.b, self._dD + self._db, lr=lr, state_bits=state_bits,
                              weight_decay=[weight_decay] * chains + [0.0] * chains)
+        self._held = ops.Held(self.D + self.b + self._dD + self._db, self.opt.device)
 
     def _check(self, scores):
         if scores.dim() != 3 or scores.shape[0] != self.chains or \
                 scores.shape[2] != self.n_class or scores.dtype != self.torch.float32:
             raise BartError(BART_EINVAL, f"scores must be float32 [{self.chains}, rows, "
                                          f"{self.n_class}]")
+        self._held.use(self.torch.cuda.current_stream(self.opt.device))
 
     def logits(self, scores, chain: int):
         return self.torch.addmm(scores[chain], scores[chain], self.D[chain].t()).add_(

@@ -177,6 +177,23 @@ def _call(device, f, *args):
             _check(f(*args, torch.cuda.current_stream(device).cuda_stream))
 
 
+class Held:
+    """Device memory that calls use and whose user does not see it: the allocator
+    is told of every other stream it is used on than the one it was made on, so
+    that memory dropped behind such a call is not handed out before the call is
+    done."""
+
+    def __init__(self, tensors, device):
+        self.tensors = [t for t in tensors if t is not None and t.numel()]
+        self.streams = {torch.cuda.current_stream(device).cuda_stream}
+
+    def use(self, stream) -> None:
+        if stream.cuda_stream not in self.streams:
+            for t in self.tensors:
+                t.record_stream(stream)
+            self.streams.add(stream.cuda_stream)
+
+
 def logprob(scores, labels=None, *, mask=None, temperature: float = 1.0, k: int = 0,
             entropy: bool = False, norm: bool = False, grad_logp=None, grad_entropy=None,
             grad_out=None) -> LogProb:
@@ -281,14 +298,19 @@ class AdamW:
         n = len(params)
         self.params, self.grads, self.state_bits, self.steps = params, grads, state_bits, int(steps)
         self.lr, self.betas, self.eps = float(lr), (float(betas[0]), float(betas[1])), float(eps)
+        made = []
         if isinstance(masters, str):
             if masters != "new":
                 _refuse('masters must be None, "new" or a list')
             masters = [p.float() if p.dtype != torch.float32 else None for p in params]
+            made += masters
         self.masters = list(masters) if masters is not None else [None] * n
         wd = list(weight_decay) if hasattr(weight_decay, "__len__") else [weight_decay] * n
         scale = list(lr_scale) if hasattr(lr_scale, "__len__") else [lr_scale] * n
-        self.state = list(state) if state is not None else [self._new_state(p) for p in params]
+        if state is None:
+            state = [self._new_state(p) for p in params]
+            made += [t for s in state for t in s.values()]
+        self.state = list(state)
         if not n == len(self.masters) == len(wd) == len(scale) == len(self.state):
             _refuse("masters, weight_decay, lr_scale and state must have one entry per tensor")
         table = (AdamwTensor * n)()
@@ -303,6 +325,7 @@ class AdamW:
         L = lib()
         need = L.bart_adamw_workspace_bytes(table, n, state_bits)
         self.ws = torch.empty(max(need, 16), dtype=torch.uint8, device=dev)
+        self._held = Held(made + [self.ws], dev)
         self.h, h = None, C.c_void_p()
         with torch.cuda.device(dev):
             _check(L.bart_adamw_init(table, n, state_bits, self.ws.data_ptr(), need,
@@ -353,8 +376,9 @@ class AdamW:
         """One step on the current stream (lr: of this step alone)."""
         y = AdamwHyper(self.lr if lr is None else lr, self.betas[0], self.betas[1], self.eps,
                        grad_scale, self.steps + 1)
-        _check(lib().bart_adamw_step(self.h, y,
-                                     torch.cuda.current_stream(self.device.index).cuda_stream))
+        stream = torch.cuda.current_stream(self.device.index)
+        self._held.use(stream)
+        _check(lib().bart_adamw_step(self.h, y, stream.cuda_stream))
         self.steps += 1
 
     def close(self) -> None:
