@@ -84,6 +84,12 @@ __device__ __forceinline__ int uniform(int v) {
   return T >= 64 ? __builtin_amdgcn_readfirstlane(v) : v;
 }
 
+// The same of a word that all lanes of a whole wave agree on.
+__device__ __forceinline__ uint64_t uniform64(uint64_t v) {
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v);
+  return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(v >> 32)) << 32 | lo;
+}
+
 // A scalar that the compiler knows nothing of: addresses derived from it are
 // computed where they are used instead of being kept, one register pair each,
 // from one turn of a loop to the next.

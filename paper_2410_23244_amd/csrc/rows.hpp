@@ -8,6 +8,7 @@
 #include <stdint.h>
 
 #include "bart_ops.h"
+#include "keysearch.hpp"
 #include "lanes.hpp"
 #include "scalar.hpp"
 
@@ -203,13 +204,17 @@ __device__ __forceinline__ float max_of(float m, const Chunk<DT> (&c)[N]) {
 // is not kept.
 template <bool ENT, int DT, int N>
 __device__ __forceinline__ void sum_chunks(Stats &q, const Chunk<DT> (&c)[N], float a) {
-  float s1 = 0.f, t1 = 0.f;
+  float s1 = 0.f, t1 = 0.f, M = q.M;
+  // with and without ENT are two sides of a branch: were they seen to share their
+  // exponentials, these would all be computed before it and kept (93 -> 188
+  // registers with 64 elements a lane)
+  if (ENT) asm("" : "+v"(M));
 #pragma unroll
   for (int n = 0; n < N; ++n)
 #pragma unroll
     for (int e = 0; e < Chunk<DT>::V; e += 2) {
-      const float z0 = __builtin_fmaf(c[n].get(e), a, -q.M);
-      const float z1 = __builtin_fmaf(c[n].get(e + 1), a, -q.M);
+      const float z0 = __builtin_fmaf(c[n].get(e), a, -M);
+      const float z1 = __builtin_fmaf(c[n].get(e + 1), a, -M);
       const float p0 = exp2_fast(z0), p1 = exp2_fast(z1);
       q.s += p0;
       s1 += p1;
@@ -353,6 +358,11 @@ __device__ __forceinline__ float key_score(uint64_t k) {
   return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u);
 }
 __device__ __forceinline__ int32_t key_class(uint64_t k) { return (int32_t)~(uint32_t)k; }
+// The last class whose key with key_score(k) reaches k, which need not be a
+// key: classes end before 2^30, and the score -0, which no key has, stands for 0.
+__device__ __forceinline__ int32_t key_last(uint64_t k) {
+  return k >> 32 == 0x7fffffffu ? INT32_MAX : (int32_t)min(~(uint32_t)k, (uint32_t)INT32_MAX);
+}
 
 // Alternative c of row i, or that there is none (key 0).
 __device__ __forceinline__ void write_top(const RowsArgs &A, int64_t i, int c, uint64_t key,
@@ -397,16 +407,20 @@ __device__ __forceinline__ void top_by_rounds(const RowsArgs &A, int64_t i, cons
 // Candidates for a row's alternatives, in LDS: a list that holds every score
 // at or above a threshold that at least k scores reach.  The threshold is the
 // k-th largest of the maxima of 64 columns (lane l of every wave that works on
-// the row forms column l), so on scores in no particular order the list
-// gets about 64 ln(64 / (64 - k)) entries, 24 for k = 20; long runs of equal
-// scores overflow it, and then the alternatives are taken one by one.
+// the row forms column l; 256 columns for k > 40 on 256 lanes and more), so on
+// scores in no particular order the list gets about 64 ln(64 / (64 - k))
+// entries, 24 for k = 20.  Where more scores reach it than the list holds (long
+// runs of equal scores, large scores in fewer than k columns, k as large as the
+// number of columns), the list is made anew above a tighter threshold, a key.
+// Keys are read two at a time: at a multiple of 16 bytes by one instruction (64 of
+// 65536 x 1000 f32 398 us, 502 otherwise).
 template <int CAP>
-struct TopList {
+struct alignas(16) TopList {
   uint64_t key[CAP];
   uint32_t count;
-  uint32_t lanes;  // lanes that hold a candidate, their numbers in cols
-  float theta;     // the threshold, where not every wave finds it, and the last
-  int32_t last;    // class that passes with that very score
+  uint32_t lanes;   // lanes that hold a candidate, their numbers in cols
+  float theta;      // the threshold, where not every wave finds it
+  uint64_t least;   // the tighter one
 };
 
 // The k-th largest of 64 lanes' values, k <= 64: by k rounds while they are
@@ -456,8 +470,10 @@ __device__ __forceinline__ void list_chunk(TopList<CAP> &list, uint32_t &count,
   }
 }
 
-// Lists the scores of the chunks of the lanes that have one to list (mine).
-// cols gets those lanes' numbers.
+// Lists the scores of the chunks of the lanes that have one to list (mine),
+// spread over all lanes.  The list's count is that of all, also where it does
+// not hold them.  cols gets those lanes' numbers; list.count and list.lanes are
+// 0 before.
 template <bool TIGHT, int DT, int T, int CAP>
 __device__ __forceinline__ void list_row(const Row<DT, T> &row, int from, int to, bool mine,
                                          float theta, int last, int lane, float *cols,
@@ -492,7 +508,7 @@ __device__ __forceinline__ void list_row(const Row<DT, T> &row, int from, int to
 template <int CAP, class PUT>
 __device__ __forceinline__ void put_ranked(const TopList<CAP> &list, int lane, int T, int k,
                                            PUT put) {
-  const int n = list.count;
+  const int n = min(list.count, (uint32_t)CAP);
   for (int c = lane; c < n; c += T) {
     const uint64_t key = list.key[c];
     int rank = 0;
@@ -549,24 +565,35 @@ __device__ __forceinline__ void top_by_list(const Row<DT, T> &row, int k, int fr
     group_sync<T>();  // cols have been read
   }
   list_row<false>(row, from, to, own >= theta && own > kNegInf, theta, 0, lane, cols, list);
-  while (uniform<T>(list.count) > CAP) {
-    constexpr int kSample = 256;
-    static_assert(kSample <= CAP && kSample > BART_MAX_TOP, "a tighter threshold exists");
-    for (int c = lane; c < kSample; c += T) {
-      const uint64_t key = list.key[c];
-      int rank = 0;
+  // An overflowing list is made anew above the k-th best of its first entries:
+  // where they come in no particular order, one in 256 / k of them remains.  After
+  // kSamples such lists the threshold is searched for by counting what reaches
+  // it, at most 64 times however the scores lie.
+  constexpr int kSample = 256, kSamples = 3;
+  static_assert(kSample <= CAP && kSample > BART_MAX_TOP, "a tighter threshold exists");
+  KeySearch s{0, ~(uint64_t)0};
+  uint32_t count = uniform<T>(list.count);
+  for (int pass = 0;
+       pass < kSamples + 64 && (count > CAP || (pass > kSamples && count < (uint32_t)k)); ++pass) {
+    if (pass < kSamples) {
+      for (int c = lane; c < kSample; c += T) {
+        const uint64_t key = list.key[c];
+        int rank = 0;
 #pragma unroll 8
-      for (int q = 0; q < kSample; ++q) rank += list.key[q] > key ? 1 : 0;
-      if (rank == k - 1) {
-        list.theta = key_score(key);
-        list.last = key_class(key);
+        for (int q = 0; q < kSample; ++q) rank += list.key[q] > key ? 1 : 0;
+        if (rank == k - 1) list.least = key;
       }
+      group_sync<T>();
+      s.lo = uniform64(list.least);
     }
-    group_sync<T>();
-    theta = list.theta;
+    const uint64_t least = pass < kSamples ? s.lo : s.probe();
     if (lane == 0) list.count = list.lanes = 0;
     group_sync<T>();
-    list_row<true>(row, from, to, own >= theta, theta, list.last, lane, cols, list);
+    theta = key_score(least);
+    list_row<true>(row, from, to, own >= theta, theta, key_last(least), lane, cols, list);
+    count = uniform<T>(list.count);
+    if (pass >= kSamples) s.take(least, count, k);
+    group_sync<T>();  // the count has been read
   }
   put_ranked(list, lane, T, k, put);
 }
