@@ -25,6 +25,22 @@ namespace {
       return fail(BART_EHIP, "%s failed: %s", #expr, hipGetErrorString(e_));       \
   } while (0)
 
+// Makes a device the current one until the end of a call, for a plan that keeps
+// the device it was made on.
+struct OnDevice {
+  int before = -1;
+  hipError_t enter(int device) {
+    int now = 0;
+    if (const hipError_t e = hipGetDevice(&now); e != hipSuccess) return e;
+    if (now == device) return hipSuccess;
+    before = now;
+    return hipSetDevice(device);
+  }
+  ~OnDevice() {
+    if (before >= 0) (void)hipSetDevice(before);
+  }
+};
+
 constexpr int64_t kMaxRows = (int64_t)1 << 40;
 constexpr int64_t kMaxLd = (int64_t)1 << 40;
 
@@ -461,7 +477,8 @@ int bart_adamw_step(bart_adamw *h, const bart_adamw_hyper *y, void *stream) {
   if (!(y->eps >= 1e-37 && std::isfinite(y->eps))) return fail(BART_EINVAL, "eps must be >= 1e-37");
   if (!std::isfinite(y->grad_scale)) return fail(BART_EINVAL, "grad_scale must be finite");
   if (y->step < 1) return fail(BART_EINVAL, "step must be >= 1");
-  HIP_TRY(hipSetDevice(h->device));
+  OnDevice here;
+  HIP_TRY(here.enter(h->device));
   AdamwStep K;
   K.b1 = (float)y->beta1;
   K.c1 = (float)(1.0 - y->beta1);
