@@ -54,7 +54,8 @@ class Calibration:
                 scores.shape[2] != self.n_class or scores.dtype != self.torch.float32:
             raise BartError(BART_EINVAL, f"scores must be float32 [{self.chains}, rows, "
                                          f"{self.n_class}]")
-        self._held.use(self.torch.cuda.current_stream(self.opt.device))
+        dev = self.opt.device
+        self._held.use(dev, self.torch.cuda.current_stream(dev).cuda_stream)
 
     def logits(self, scores, chain: int):
         return self.torch.addmm(scores[chain], scores[chain], self.D[chain].t()).add_(
