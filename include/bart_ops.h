@@ -15,7 +15,9 @@
  * checked before anything is enqueued, bart_last_error() for the message, no
  * device memory allocated by the library.  Calls enqueue on the given stream
  * (a hipStream_t, NULL = default stream) and do not synchronise it, except
- * bart_adamw_init.  They can be captured into a graph.
+ * bart_adamw_init.  They can be captured into a graph, except that
+ * bart_adamw_init cannot and that a captured bart_adamw_step repeats one step
+ * (see there).
  */
 #ifndef BART_OPS_H
 #define BART_OPS_H
@@ -171,7 +173,12 @@ int bart_adamw_init(const bart_adamw_tensor *t, int32_t n_tensors, int32_t state
  * whole up to 1/16 faster in its logarithm (independent random thresholds
  * would leave no such tendency, and about five times the scatter).
  * A gradient that is NaN or infinite makes its element's state NaN; with
- * 8-bit states, possibly its whole block's. */
+ * 8-bit states, possibly its whole block's.
+ * What hyper holds is taken at the call.  A graph that captured it repeats step
+ * t at every replay: the bias corrections stand still, and with 8-bit states
+ * each element meets the same threshold again, so that a root may never move
+ * (what the sequence is there to avoid).  Training needs a call per step; the
+ * plan, its arrays and the workspace must outlive such a graph. */
 int bart_adamw_step(bart_adamw *h, const bart_adamw_hyper *hyper, void *stream);
 
 void bart_adamw_destroy(bart_adamw *h);

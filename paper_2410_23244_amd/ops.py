@@ -385,7 +385,10 @@ class AdamW:
             _refuse(f"state {i} does not fit its param and state_bits = {self.state_bits}")
 
     def step(self, lr: Optional[float] = None, grad_scale: float = 1.0) -> None:
-        """One step on the current stream (lr: of this step alone)."""
+        """One step on the current stream (lr: of this step alone).  A graph that
+        captured it repeats this one step, with its number, lr and grad_scale, at
+        every replay, and needs this object as long as it is replayed: train by
+        calls, not by replays."""
         y = AdamwHyper(self.lr if lr is None else lr, self.betas[0], self.betas[1], self.eps,
                        grad_scale, self.steps + 1)
         # the handle alone: a stream's object takes 1.1 us of the 5 of a small step
