@@ -265,6 +265,8 @@ def logprob_grad(scores, labels, norm, grad_logp, *, entropy=None, grad_entropy=
 
 def _dense(t: torch.Tensor) -> bool:
     """Whether the elements fill one stretch of memory, in any order of dimensions."""
+    if t.numel() == 0:
+        return True
     need = 1
     for size, stride in sorted(((s, st) for s, st in zip(t.shape, t.stride()) if s != 1),
                                key=lambda q: q[1]):
@@ -272,6 +274,12 @@ def _dense(t: torch.Tensor) -> bool:
             return False
         need *= size
     return True
+
+
+def _same_layout(a: torch.Tensor, b: torch.Tensor) -> bool:
+    """Whether two dense tensors of one shape hold their elements in one order."""
+    return a.shape == b.shape and (a.stride() == b.stride() or a.numel() == 0 or all(
+        s == 1 or x == y for s, x, y in zip(a.shape, a.stride(), b.stride())))
 
 
 def _ptr(t):
@@ -359,8 +367,7 @@ class AdamW:
 
     def _check_tensor(self, i, p, g, w, s):
         def same(t, dtype):
-            return (t.dtype == dtype and t.shape == p.shape and t.stride() == p.stride() and
-                    t.device == self.device)
+            return t.dtype == dtype and _same_layout(t, p) and t.device == self.device
 
         def flat(t, dtype, n):
             return (t.dtype == dtype and t.shape == (n,) and t.is_contiguous() and

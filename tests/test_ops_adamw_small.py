@@ -58,3 +58,18 @@ def test_tiny_second_moments(ops, pdt, gdt, n, every):
         assert np.isfinite(got).all()
         assert (np.abs(opt.state[0]["v"].double().cpu().numpy() - v) <= e_v).all()
     assert n < 100 or (ok & (v < 2.0 ** -126)).sum() > n / (3 * every)   # tiny ones among them
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_empty_tensors_and_dimensions_of_size_one(ops, bits):
+    """A 1 x 1 convolution's weights and their gradients are of one layout whatever
+    the strides of the two last dimensions say; a tensor without elements is dense."""
+    def conv(x):
+        return torch.as_strided(x.clone(), (8, 3, 1, 1), (3, 1, 3, 3))
+
+    w, g = torch.randn(24, device="cuda"), torch.randn(24, device="cuda")
+    a = [torch.as_strided(w.clone(), (8, 3, 1, 1), (3, 1, 1, 1)), torch.empty(5, 0, device="cuda")]
+    b = [w.clone()]
+    ops.AdamW(a, [conv(g), torch.empty(5, 0, device="cuda")], state_bits=bits).step()
+    ops.AdamW(b, [g], state_bits=bits).step()
+    assert torch.equal(a[0].reshape(-1), b[0]) and not torch.equal(b[0], w)
