@@ -152,8 +152,8 @@ size_t bart_adamw_workspace_bytes(const bart_adamw_tensor *t, int32_t n_tensors,
 
 /* A plan over n_tensors >= 1 tensors (host array, copied; the device arrays
  * it names are borrowed and must outlive the plan, as must the workspace,
- * 16-byte aligned).  state_bits: 32 or 8.  Arrays of different tensors must
- * not overlap.  Synchronises the stream.  Steps run on the device that is
+ * 16-byte aligned).  state_bits: 32 or 8.  No array that is written may overlap
+ * one of another tensor (BART_EINVAL).  Synchronises the stream.  Steps run on the device that is
  * current now, whichever is current then; they leave it current. */
 int bart_adamw_init(const bart_adamw_tensor *t, int32_t n_tensors, int32_t state_bits,
                     void *workspace, size_t ws_bytes, void *stream, bart_adamw **out);

@@ -6,6 +6,7 @@
 #include <cmath>
 #include <cstring>
 #include <exception>
+#include <iterator>
 #include <vector>
 
 #include "adamw.hpp"
@@ -328,6 +329,49 @@ const char *check_tensors(const bart_adamw_tensor *t, int32_t n, int32_t bits) {
   return nullptr;
 }
 
+// Whether an array that one tensor's step writes shares memory with an array of
+// another tensor.  (Two tensors may have one gradient.)
+bool tensors_overlap(const bart_adamw_tensor *t, int32_t n, int32_t bits) {
+  struct Range {
+    uintptr_t from, to;
+    int32_t tensor;
+  };
+  std::vector<Range> out, in;
+  for (int32_t i = 0; i < n; ++i) {
+    const bart_adamw_tensor &q = t[i];
+    if (q.n == 0) continue;
+    const int64_t state = bits == 32 ? 4 : 1, blocks = (q.n + kStateBlock - 1) / kStateBlock;
+    auto add = [&](std::vector<Range> &to, const void *p, int64_t bytes) {
+      if (p) to.push_back({(uintptr_t)p, (uintptr_t)p + (uintptr_t)bytes, i});
+    };
+    add(out, q.param, q.n * dtype_bytes(q.param_dtype));
+    add(out, q.master, q.n * 4);
+    add(out, q.m, q.n * state);
+    add(out, q.v, q.n * state);
+    add(out, q.m_scale, blocks * 4);
+    add(out, q.v_scale, blocks * 4);
+    add(in, q.grad, q.n * dtype_bytes(q.grad_dtype));
+  }
+  auto before = [](const Range &a, const Range &b) { return a.from < b.from; };
+  std::sort(out.begin(), out.end(), before);
+  std::vector<Range> parts;  // apart and in order; a tensor's own ones that touch are one
+  for (const Range &r : out) {
+    if (!parts.empty() && r.from < parts.back().to) {
+      if (r.tensor != parts.back().tensor) return true;
+      parts.back().to = std::max(parts.back().to, r.to);
+    } else {
+      parts.push_back(r);
+    }
+  }
+  for (const Range &r : in) {
+    auto p = std::upper_bound(parts.begin(), parts.end(), r, before);
+    if (p != parts.begin() && std::prev(p)->to > r.from) --p;
+    for (; p != parts.end() && p->from < r.to; ++p)
+      if (p->tensor != r.tensor) return true;
+  }
+  return false;
+}
+
 // The kernels differ by the types of a tensor: tensors of equal types form a
 // group, and a group is one launch.
 int group_of(const bart_adamw_tensor &t) { return t.param_dtype * 2 + (t.grad_dtype != t.param_dtype); }
@@ -427,12 +471,14 @@ int bart_adamw_init(const bart_adamw_tensor *t, int32_t n_tensors, int32_t state
   *out = nullptr;
   if (const char *e = check_tensors(t, n_tensors, state_bits)) return fail(BART_EINVAL, "%s", e);
   if (!workspace) return fail(BART_EINVAL, "workspace is NULL");
-  if ((uintptr_t)workspace % 16) return fail(BART_ENOSPACE, "workspace must be 16-byte aligned");
-  const size_t need = bart_adamw_workspace_bytes(t, n_tensors, state_bits);
-  if (ws_bytes < need)
-    return fail(BART_ENOSPACE, "workspace holds %zu bytes, %zu are needed", ws_bytes, need);
   bart_adamw *h = nullptr;
   try {
+    if (tensors_overlap(t, n_tensors, state_bits))
+      return fail(BART_EINVAL, "arrays of different tensors overlap");
+    if ((uintptr_t)workspace % 16) return fail(BART_ENOSPACE, "workspace must be 16-byte aligned");
+    const size_t need = bart_adamw_workspace_bytes(t, n_tensors, state_bits);
+    if (ws_bytes < need)
+      return fail(BART_ENOSPACE, "workspace holds %zu bytes, %zu are needed", ws_bytes, need);
     h = new bart_adamw;
     std::vector<AdamwChunk> chunks;
     chunks.reserve((need - table_bytes(n_tensors)) / sizeof(AdamwChunk));
