@@ -113,13 +113,19 @@ class Classifier:
             raise BartError(BART_EINVAL, "y must be classes 0, 1, ... of at least 2 observations")
         if not 0.0 < self.holdout < 1.0:
             raise BartError(BART_EINVAL, "holdout must be between 0 and 1")
+        X, X_test = np.asarray(X, dtype=np.float32), np.asarray(X_test, dtype=np.float32)
+        if X.ndim != 2 or X_test.ndim != 2 or X.shape[0] != y.size or \
+                X.shape[1] != X_test.shape[1]:
+            raise BartError(BART_EINVAL, "X must have one row per class in y, X_test X's columns")
+        if n_burn < 0 or n_keep < 1:
+            raise BartError(BART_EINVAL, "n_burn must be >= 0 and n_keep >= 1")
         self.n_class = max(int(y.max()) + 1, 2)
         rng = np.random.default_rng([self.seed, 8])
         order = rng.permutation(y.size)
         n_held = min(max(1, int(round(self.holdout * y.size))), y.size - 1)
         held, kept = order[:n_held], order[n_held:]
-        Xt = np.ascontiguousarray(np.asarray(X, dtype=np.float32).T)
-        Xs = np.ascontiguousarray(np.asarray(X_test, dtype=np.float32).T)
+        Xt = np.ascontiguousarray(X.T)
+        Xs = np.ascontiguousarray(X_test.T)
         self.cuts, self.n_cuts = bart_cutpoints(Xt[:, kept], self.K, self.grid)
         Xb = bart_bin(Xt[:, kept], self.cuts, self.n_cuts)
         points = bart_bin(np.concatenate([Xt[:, held], Xs], axis=1), self.cuts, self.n_cuts)
@@ -153,10 +159,14 @@ class Classifier:
         return self
 
     def answer(self, y_test=None, k: int = 1) -> ops.LogProb:
-        """The calibrated answers at the test points (ops.LogProb)."""
+        """The calibrated answers at the test points (ops.LogProb); y_test: their
+        classes, negative where there is none (one that was not fitted has logp NaN)."""
         import torch
 
         label = None
         if y_test is not None:
-            label = torch.from_numpy(np.asarray(y_test, dtype=np.int64)).to(self.scores.device)
+            y = np.asarray(y_test)
+            if y.shape != (self.scores.shape[1],) or not np.issubdtype(y.dtype, np.integer):
+                raise BartError(BART_EINVAL, "y_test must be a class for each test point")
+            label = torch.from_numpy(y.astype(np.int64)).to(self.scores.device)
         return self.calibration.answer(self.scores, label, k=min(k, self.n_class))
