@@ -249,6 +249,8 @@ def logprob_grad(scores, labels, norm, grad_logp, *, entropy=None, grad_entropy=
     temperature."""
     r = _rows(scores, labels, mask, temperature)
     n = r.n
+    if norm is None:
+        _refuse("the gradient alone needs the norm that logprob returned")
     for name, t, shape in (("norm", norm, (n, 2)), ("entropy", entropy, (n,))):
         if t is not None and (t.dtype != torch.float32 or t.shape != shape or
                               t.device != scores.device or not t.is_contiguous()):

@@ -56,3 +56,8 @@ def test_layouts_are_compared_where_they_matter():
     assert not same(_t((3, 4), (4, 1)), _t((3, 4), (1, 3)))
     assert not same(_t((4, 3), (3, 1)), _t((3, 4), (4, 1)))
     assert not same(_t((5, 0), (1, 1)), _t((0, 5), (1, 1)))
+
+
+def test_a_gradient_alone_needs_what_was_kept():
+    with pytest.raises(BartError):
+        ops.logprob_grad(_scores(3, 7), None, None, None)
