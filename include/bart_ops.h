@@ -61,7 +61,8 @@ typedef struct {
   const float *w_entropy; /* device, w_entropy[i * w_entropy_stride] */
   int64_t w_entropy_stride;
   void *grad;             /* device [n][ld_grad] of the scores' dtype; may be the scores
-                             themselves (same ld, not 0), else apart from them */
+                             themselves (same ld, not 0) or lie between their rows (same
+                             ld), else apart from them */
   int64_t ld_grad;        /* >= n_class */
 } bart_rows_grad;
 

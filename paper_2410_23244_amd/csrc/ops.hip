@@ -51,6 +51,15 @@ bool overlap(const void *a, int64_t abytes, const void *b, int64_t bbytes) {
   return x < y + (uintptr_t)bbytes && y < x + (uintptr_t)abytes;
 }
 
+// Whether rows of `row` bytes that begin `stride` bytes apart at a lie in the gaps
+// between such rows at b.
+bool between(const void *a, const void *b, int64_t row, int64_t stride) {
+  if (stride == 0) return false;
+  const int64_t off = (int64_t)((uintptr_t)a - (uintptr_t)b) % stride;
+  const int64_t at = off < 0 ? off + stride : off;
+  return at >= row && at <= stride - row;
+}
+
 // Whether n steps of a stride reach past what an address computation holds.
 bool too_far(int64_t n, int64_t stride) { return stride > 0 && n > ((int64_t)1 << 60) / stride; }
 
@@ -89,7 +98,8 @@ const char *check_grad(const bart_rows *r, const bart_rows_grad *g) {
   if (r->n == 0) return nullptr;
   const int64_t es = dtype_bytes(r->dtype);
   const bool same = g->grad == r->x && (g->ld_grad == r->ld || r->n == 1);
-  if (!same && overlap(r->x, ((r->n - 1) * r->ld + r->n_class) * es, g->grad,
+  const bool apart = g->ld_grad == r->ld && between(g->grad, r->x, r->n_class * es, r->ld * es);
+  if (!same && !apart && overlap(r->x, ((r->n - 1) * r->ld + r->n_class) * es, g->grad,
                        ((r->n - 1) * g->ld_grad + r->n_class) * es))
     return "grad overlaps the scores without being them";
   return nullptr;
