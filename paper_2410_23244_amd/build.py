@@ -29,8 +29,8 @@ def build(verbose: bool = False, extra: list[str] | None = None, clocks: bool = 
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     out = CLOCKS_LIB if clocks else LIB
     tmp = out + ".tmp"
-    cmd = [hipcc, *FLAGS, *(["-DBART_PHASE_CLOCKS"] if clocks else []), *(extra or []), "-parallel-jobs=2",
-           *(SRCS[:1] if clocks else SRCS), "-o", tmp]
+    cmd = [hipcc, *FLAGS, *(["-DBART_PHASE_CLOCKS"] if clocks else []), *(extra or []),
+           "-parallel-jobs=2", *(SRCS[:1] if clocks else SRCS), "-o", tmp]
     if verbose:
         print(" ".join(cmd), flush=True)
     res = subprocess.run(cmd, capture_output=True, text=True)

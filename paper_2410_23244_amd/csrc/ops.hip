@@ -138,7 +138,7 @@ int64_t span_of(const bart_rows &r) {
 //    a gradient 101 / 113, f32 94 / 86 and 210 / 188, with 5 alternatives 109 /
 //    127;
 //  - 16384 with a gradient: 64 a lane of 256 against a stream: 8192 x 16384
-//    f32 204 / 239; without one a stream is as fast (94);
+//    f32 209 / 239; without one a stream is as fast (94);
 //  - 32768 with a gradient: 64 a lane of 512 against 32 of 1024: 8192 x 32768
 //    bf16 194 / 224, f32 (twice the registers) 4096 x 32768 230 / 195;
 //  - beyond: a stream that holds a part against 64 a lane of 1024: 8192 x 50001
@@ -185,12 +185,17 @@ RowsLaunch grad_in_registers(const RowsArgs &A) {
 }
 
 // Few long rows are split over workgroups: parts of a row and classes of a
-// part (S = 1: not split).  A second launch joins the parts, which also costs
-// the caller 3 us, so it pays where one workgroup would read for long: 131072
-// bf16 classes, us on the device of 1 / 32 / 64 / 128 rows: split 5.2 / 6.3 / 8.4
-// / 11.7, a row per workgroup 10 / 10 / 11 / 12; 100000 classes, 1 row, without
-// and with 20 alternatives: 5.1 and 11.4, 9.8 and 14.6; 65536: 5.3 and 11.7, 6.7
-// and 10.7.
+// part (S = 1: not split).  A second launch joins the parts, and a gradient is a
+// third; each also costs the caller 3 us, so it pays where one workgroup would
+// read for long: 131072 bf16 classes, us on the device of 1 / 32 / 64 / 128
+// rows: split 5.2 / 6.3 / 8.4 / 11.7, a row per workgroup 10 / 10 / 11 / 12;
+// 100000 classes, 1 row, without and with 20 alternatives: 5.1 and 11.4, 9.8 and
+// 14.6.  At 65536, forward / with 20 alternatives / with the gradient, split
+// against a row per workgroup: 1 row bf16 5.3 / 11.6 / 8.8 against 6.6 / 10.4 /
+// 10.0, f32 5.0 / 10.8 / 8.4 against 6.7 / 10.8 / 11.8; 64 rows bf16 6.4 / 12.6 /
+// 11.7 against 7.3 / 11.6 / 11.5, f32 7.6 / 13.6 / 15.8 against 8.0 / 12.4 / 14.3.
+// What up to 16 rows without alternatives gain there is less than the launches
+// cost; at 40000 classes the gain is below 1 us and alternatives lose 2 to 3.
 struct Split {
   int S, length;
 };
@@ -323,7 +328,8 @@ const char *check_tensors(const bart_adamw_tensor *t, int32_t n, int32_t bits) {
     if (!dtype_ok(q.param_dtype)) return "param_dtype must be BART_F32, BART_F16 or BART_BF16";
     if (q.grad_dtype != q.param_dtype && q.grad_dtype != BART_F32)
       return "grad_dtype must be param_dtype or BART_F32";
-    if (q.master && q.param_dtype == BART_F32) return "a master copy stands beside 16-bit weights only";
+    if (q.master && q.param_dtype == BART_F32)
+      return "a master copy stands beside 16-bit weights only";
     if (!std::isfinite(q.weight_decay)) return "weight_decay must be finite";
     if (!std::isfinite(q.lr_scale)) return "lr_scale must be finite";
     if (q.n == 0) continue;

@@ -159,8 +159,8 @@ struct Row {
 // Scores far below -2^26 (masks by large negative numbers) then have z far below 0
 // and count for nothing; where they are all that a row has, or the largest is
 // above 2^26, m a and M are apart by more than rounding (at most 4), and the
-// row is summed again by differences x - m (`careful`).  A NaN among the scores shows as s = NaN, and a row
-// without any as m = -inf.
+// row is summed again by differences x - m (`careful`).  A NaN among the scores
+// shows as s = NaN, and a row without any as m = -inf.
 
 constexpr float kMostRef = 0x1p26f;
 
@@ -267,7 +267,8 @@ struct RowEnd {
 // Sums a row that has a score above -inf and no NaN by differences x - m,
 // element by element.
 template <int DT, int T>
-__device__ __forceinline__ RowEnd careful(const Row<DT, T> &row, float inv_t, int lane, Stats *part) {
+__device__ __forceinline__ RowEnd careful(const Row<DT, T> &row, float inv_t, int lane,
+                                          Stats *part) {
   constexpr int W = T > 64 ? T / 64 : 1, L = T > 64 ? 64 : T;
   auto all_max = [&](float v) {
     v = lanes_max<L>(v);
@@ -374,7 +375,8 @@ __device__ __forceinline__ void write_top(const RowsArgs &A, int64_t i, int c, u
 }
 
 // The alternatives of a row by T < 64 lanes that hold it in registers (a
-// lane's chunks begin with classes j0, j0 + T V, ...), one after the other: the largest score, its lowest class, then without it.
+// lane's chunks begin with classes j0, j0 + T V, ...), one after the other: the
+// largest score, its lowest class, then without it.
 template <int DT, int N, int T>
 __device__ __forceinline__ void top_by_rounds(const RowsArgs &A, int64_t i, const Row<DT, T> &row,
                                               const RowEnd &r, const Chunk<DT> (&c)[N], int lane,
@@ -773,7 +775,7 @@ __global__ __launch_bounds__(T > 256 ? T : 256) void k_rows(RowsArgs A, const fl
 
 // Rows of any length: T lanes read a row's chunks 4 at a time, and a second
 // time for the gradient, except the last H chunks of each lane, which stay in
-// registers.  Bound by memory: 16384 x 131072 bf16 698 us (6.15 TB/s at 8
+// registers.  Bound by memory: 16384 x 131072 bf16 701 us (6.1 TB/s at 8
 // instructions per score); with the gradient by what is read twice, which
 // reaches the caches beyond the compute unit's own at the rate of memory:
 // 8192 x 50001 bf16 361 us (4.5 TB/s of operands).
@@ -839,8 +841,8 @@ __global__ __launch_bounds__(T) void k_rows_stream(RowsArgs A) {
 // Few long rows: each row's chunks are split over S workgroups of 256 lanes,
 // `length` classes (a multiple of 256 V) each, that leave their statistics
 // and their k best keys in part [n][S] and keys [n][S][k].  Bound by latency:
-// one row of 131101 bf16 classes 3.4 us here and 2.4 in the join, 8.4 and 4.7
-// with 20 alternatives.
+// one row of 131101 bf16 classes 3.4 us here and 2.4 in the join, 8.3 and 4.2
+// with 20 alternatives, whose candidates are read again and ranked here.
 template <int DT>
 __global__ __launch_bounds__(256) void k_rows_part(RowsArgs A, int S, int length, Stats *part_out,
                                                   uint64_t *keys) {

@@ -293,11 +293,11 @@ class AdamW:
 
     params, grads: lists of dense tensors, pairwise of one shape and layout,
     on one device and apart from each other (a shared weight is given once);
-    params float32, float16 or bfloat16, grads of the param's dtype or float32.  They are updated and read in place: a step uses what
-    the grads hold when it runs.  masters: None, or for 16-bit params a list of
-    float32 tensors that hold the weights, of which the params are then
-    rounded copies ("new" makes them from the params).  weight_decay, lr_scale:
-    a number, or one for each tensor.
+    params float32, float16 or bfloat16, grads of the param's dtype or float32.
+    They are updated and read in place: a step uses what the grads hold when it
+    runs.  masters: None, or for 16-bit params a list of float32 tensors that hold
+    the weights, of which the params are then rounded copies ("new" makes them
+    from the params).  weight_decay, lr_scale: a number, or one for each tensor.
 
     state_bits 32: float32 moments, state[i]["m"] and ["v"].  state_bits 8:
     float8_e4m3fn state[i]["m"] and ["r"] (the ROOT of the second moment),
