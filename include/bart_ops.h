@@ -139,9 +139,9 @@ typedef struct {
 } bart_adamw_tensor;
 
 typedef struct {
-  double lr, beta1, beta2; /* lr finite; betas in [0, 1) */
+  double lr, beta1, beta2; /* lr finite as f32; betas in [0, 1) */
   double eps;              /* >= 1e-37 */
-  double grad_scale;       /* gradients are multiplied by it first */
+  double grad_scale;       /* finite as f32: gradients are multiplied by it first */
   int64_t step;            /* t >= 1, the number of this step */
 } bart_adamw_hyper;
 

@@ -533,11 +533,12 @@ int bart_adamw_init(const bart_adamw_tensor *t, int32_t n_tensors, int32_t state
 int bart_adamw_step(bart_adamw *h, const bart_adamw_hyper *y, void *stream) {
   if (!h) return fail(BART_EINVAL, "plan is NULL");
   if (!y) return fail(BART_EINVAL, "hyper is NULL");
-  if (!std::isfinite(y->lr)) return fail(BART_EINVAL, "lr must be finite");
+  if (!std::isfinite((float)y->lr)) return fail(BART_EINVAL, "lr must be finite in 32 bits");
   if (!(y->beta1 >= 0.0 && y->beta1 < 1.0 && y->beta2 >= 0.0 && y->beta2 < 1.0))
     return fail(BART_EINVAL, "betas must be in [0, 1)");
   if (!(y->eps >= 1e-37 && std::isfinite(y->eps))) return fail(BART_EINVAL, "eps must be >= 1e-37");
-  if (!std::isfinite(y->grad_scale)) return fail(BART_EINVAL, "grad_scale must be finite");
+  if (!std::isfinite((float)y->grad_scale))
+    return fail(BART_EINVAL, "grad_scale must be finite in 32 bits");
   if (y->step < 1) return fail(BART_EINVAL, "step must be >= 1");
   OnDevice here;
   HIP_TRY(here.enter(h->device));

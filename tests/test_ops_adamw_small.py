@@ -73,3 +73,17 @@ def test_empty_tensors_and_dimensions_of_size_one(ops, bits):
     ops.AdamW(a, [conv(g), torch.empty(5, 0, device="cuda")], state_bits=bits).step()
     ops.AdamW(b, [g], state_bits=bits).step()
     assert torch.equal(a[0].reshape(-1), b[0]) and not torch.equal(b[0], w)
+
+
+@pytest.mark.parametrize("kw", [dict(grad_scale=1e39), dict(grad_scale=-1e300), dict(lr=1e39)])
+def test_rates_that_32_bits_do_not_hold(ops, kw):
+    """Infinite there, such a factor makes NaN of every gradient of 0."""
+    from paper_2410_23244_amd.bart import BartError
+
+    p, g = torch.ones(5, device="cuda"), torch.zeros(5, device="cuda")
+    opt = ops.AdamW([p], [g])
+    with pytest.raises(BartError):
+        opt.step(**kw)
+    assert opt.steps == 0
+    opt.step(grad_scale=3e38)
+    assert (p == 1).all()
